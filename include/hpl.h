@@ -420,10 +420,9 @@ int hpl_token_logprobs_with_grad(const hpl_logprobs_args* args, void* cuda_strea
 /* Orthogonalisation by Newton-Schulz products.  For every matrix U of the batch, X = U / (|U|_F + eps) and then `steps` times
  *     X <- a X + b (X X^T) X + c (X X^T)^2 X,        (a, b, c) = (3.4445, -4.7750, 2.0315),
  * which takes the singular values towards 1 and leaves the singular vectors.  A zero matrix stays zero, elements of
- * X below 2^-38 count as zero; NaN or infinity in U gives NaN.  Products are taken on the side of the smaller Gram matrix.  An fp32 result has 32-bit arithmetic throughout;
- * a bf16 result is computed with an error below its own rounding (up to 1e-2 of
- * its norm for large matrices of many equal entries).  On a device wait that expires (it does not in a correct
- * run) the result is NaN. */
+ * X below 2^-38 count as zero; NaN or infinity in U gives NaN.  Products are taken on the side of the smaller Gram matrix.  Arithmetic
+ * is 32-bit throughout, whatever the result's type: a bf16 result is rounded once, at the end.  On a device wait that expires (it does
+ * not in a correct run) the result is NaN. */
 #define HPL_ORTHO_MAX_BATCH  65535
 #define HPL_ORTHO_MAX_SIDE   (1ll << 17)
 #define HPL_ORTHO_MAX_ELEMENTS (1ll << 33)   /* of one matrix */

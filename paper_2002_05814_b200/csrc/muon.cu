@@ -9,12 +9,10 @@
 // 480-fold at the end: X in one 16-bit plane is not enough.  X, A and P are held as two fp16 planes, hi + lo, of the value
 // times 2^14 (|X| <= 1.21, |A| <= 1.47, |P| <= 2.81 by the polynomial's range, so hi stays below 65504; the pair resolves
 // 22 bits down to 2^-38).  A product of pairs is three tensor-core products, hi hi + hi lo + lo hi, in one fp32
-// accumulator: 32-bit results.  For a 16-bit result of a side above 256, products take hi hi alone, except A A in the last
-// two steps; the sums a X and b A keep both planes, so that the dropped terms pass through P only, and roundings average out.
-// What is left is at most 1.6e-3 of the result's norm over Gaussian, heavy-tailed, low-rank and decaying spectra of sides from
-// 260 (single products throughout: 3.1e-3; triple ones throughout the last two steps: 8e-4 for 1.6 times the work), below the
-// bf16 rounding of the result itself (1.7e-3); a matrix of many equal entries, whose roundings are all the same, can reach
-// 1e-2.  Smaller matrices average less (5e-3 for a single entry) and have little to gain: always three products.
+// accumulator: 32-bit results, for a 16-bit result too, whose only rounding that counts is then the last one (1.7e-3 of its norm).  Products
+// of the hi planes alone would take a third of the tensor cores' work, but their 11 bits are seen: 1.6e-3 of the norm over a Gaussian
+// matrix after 5 steps, where roundings average out, 3e-3 to 6e-3 where they do not (few rows that are not zero, equal entries, a
+// single entry), and more with every further step (300 x 500 Gaussian: 4.6e-3 after 8, 1.4e-2 after 64).
 #include <cooperative_groups.h>
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -37,12 +35,11 @@ constexpr double kLeastNorm = 1e-34;         // |U| + eps at least, so that kPla
 constexpr float kPlane = 16384.f;            // planes hold value * 2^14
 constexpr float kUnplane = 1.f / 16384.f;
 constexpr int kTileM = 128, kTileK = 64;
-constexpr int kChunk = 2;                    // blocks of 64 k between two readings of the accumulator (triple products)
+constexpr int kChunk = 2;                    // blocks of 64 k between two readings of the accumulator
 constexpr int kBoxBytes = 64 * 128;          // a TMA box: 64 rows of 64 fp16, 128-byte swizzle
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = (kEpiWarps + 4) * 32;   // whole warpgroups: loads and products have one of their own
 constexpr int kBlockWords = 32 * 32;         // an epilogue warp's transposition block
-constexpr int kSingleSide = 256;             // 16-bit results: single products above this side
 constexpr int kPartials = 1024;               // at most so many partial sums of squares per matrix
 
 // The three products of a step; the last one of the last step makes the result.
@@ -73,7 +70,6 @@ struct NsParams {
     Planes x[2], a, p;
     Output out;
     int32_t rows, cols, side, batch, steps;
-    int32_t single;         // 16-bit result: single products (but A A in the last two steps)
     int32_t phase;          // 3 step + op
     int32_t split;          // CTAs (a cluster) that share the sum over k of a tile; then there is one tile for each cluster
 };
@@ -155,7 +151,7 @@ struct Phase {
     const Planes *src, *dst;    // the addend (none: null); where planes go (the result: null)
     int32_t M, N, K;
     int32_t a_mn, b_mn;         // operand stored with its M (N) dimension contiguous instead of K
-    int32_t symmetric, prod;
+    int32_t symmetric;
     float alpha, beta;          // alpha D + beta addend
     int32_t tiles_m, tiles_n, tiles;   // of one matrix
 };
@@ -181,7 +177,6 @@ __host__ __device__ inline Phase phase_at(const NsParams& g, int phase, int bm, 
     const int step = phase / 3, op = phase % 3, cur = step & 1;
     const bool wide = g.rows <= g.cols;
     Phase f = {};
-    f.prod = g.single && !(op == kPoly && step >= g.steps - 2) ? 1 : 3;
     f.M = f.N = f.K = g.side;
     f.symmetric = op != kApply;
     if (op == kGram) {          // A = X X^T, or X^T X with both operands' M (N) contiguous
@@ -243,13 +238,8 @@ struct Config {
     static constexpr int kABytes = kTileM * 128, kBBytes = kBRows * 128;    // of a plane, 64 k
     static constexpr int kScratch = kEpiWarps * kBlockWords * 4;
     static constexpr int kRing = (227 << 10) - 1024 - 512 - kScratch;
-    static constexpr int kMaxStages = 6;
     static constexpr size_t kSmem = 1024 + (size_t)kRing + kScratch + 512;
-    // as many stages as fit: pairs of planes take twice the room
-    __host__ __device__ static constexpr int stages(int planes) {
-        const int n = kRing / ((kABytes + kBBytes) * planes);
-        return n < kMaxStages ? n : kMaxStages;
-    }
+    static constexpr int kStageBytes = (kABytes + kBBytes) * 2, kStages = kRing / kStageBytes;   // as many as fit: 3 or 4
 };
 
 // Two values as a word of hi parts and a word of lo parts.
@@ -301,10 +291,10 @@ __device__ __forceinline__ void write_result(const Output& o, int64_t at, int n,
 }
 
 // Products, and what follows them.  Warps 0-7: epilogue; 8: loads; 9: tensor-core products.
-template <int CTAS, int BN, int MODE, int PROD>
+template <int CTAS, int BN, int MODE>
 __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_constant__ NsParams g) {
     using C = Config<CTAS, BN>;
-    constexpr int kTmemCols = 2 * BN, kMaxStages = C::kMaxStages;
+    constexpr int kTmemCols = 2 * BN, kStageBytes = C::kStageBytes, kStages = C::kStages;
     extern __shared__ uint8_t raw[];
     uint8_t* base = (uint8_t*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);   // the swizzle repeats every 1024 bytes
     uint4* scratch = (uint4*)(base + C::kRing / 1024 * 1024);
@@ -312,11 +302,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
     // full[stage], empty[stage], accumulator full[2], accumulator empty[2]
     const uint32_t bar0 = smem_addr(bars);
     auto full = [&](int s) { return bar0 + 8 * s; };
-    auto empty = [&](int s) { return bar0 + 8 * (kMaxStages + s); };
-    auto acc_full = [&](int s) { return bar0 + 8 * (2 * kMaxStages + s); };
-    auto acc_empty = [&](int s) { return bar0 + 8 * (2 * kMaxStages + 2 + s); };
-    volatile int* abort = (volatile int*)(bars + 2 * kMaxStages + 4);
-    uint32_t* tmem_slot = (uint32_t*)(bars + 2 * kMaxStages + 5);
+    auto empty = [&](int s) { return bar0 + 8 * (kStages + s); };
+    auto acc_full = [&](int s) { return bar0 + 8 * (2 * kStages + s); };
+    auto acc_empty = [&](int s) { return bar0 + 8 * (2 * kStages + 2 + s); };
+    volatile int* abort = (volatile int*)(bars + 2 * kStages + 4);
+    uint32_t* tmem_slot = (uint32_t*)(bars + 2 * kStages + 5);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     uint32_t cta = 0;       // which of the pair
     int part = 0;           // which of those that share a sum
@@ -325,7 +315,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
 
     if (threadIdx.x == 0) {
         *abort = 0;
-        for (int s = 0; s < kMaxStages; ++s) {
+        for (int s = 0; s < kStages; ++s) {
             mbar_init(full(s), 1);
             mbar_init(empty(s), 1);
         }
@@ -354,13 +344,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
     asm volatile("griddepcontrol.wait;" ::: "memory");        // what earlier kernels wrote is read from here on
 
     // The tensor core's fp32 accumulator cuts off what does not fit, always towards zero: over 256 additions that is 1e-5 of a
-    // sum of squares.  Triple products therefore leave it every 2 blocks (24 additions, 8 of them onto a sum that matters) and
+    // sum of squares.  Products therefore leave it every 2 blocks (24 additions, 8 of them onto a sum that matters) and
     // are summed up in registers, rounded to nearest.
     const Phase f = phase_at(g, g.phase, CTAS * kTileM, BN);
     const int all_blocks = (f.K + kTileK - 1) / kTileK, per_part = (all_blocks + g.split - 1) / g.split;
     const int first_block = part * per_part, k_blocks = min(per_part, all_blocks - first_block);    // of 64 k, this CTA's
-    const int chunk = PROD == 3 ? kChunk : k_blocks;
-    constexpr int kLoaded = PROD == 3 ? 2 : 1, kStageBytes = (C::kABytes + C::kBBytes) * kLoaded, kStages = C::stages(kLoaded);
     struct Ring {
         int stage = 0;
         uint32_t phase = 0;
@@ -378,9 +366,9 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
                         const uint32_t dst = smem_addr(base) + ring.stage * kStageBytes;
                         const uint32_t bar = CTAS == 2 ? leader_addr(full(ring.stage)) : full(ring.stage);
                         if (cta == 0) mbar_expect(full(ring.stage), CTAS * kStageBytes);
-                        for (int pl = 0; pl < kLoaded; ++pl) {
+                        for (int pl = 0; pl < 2; ++pl) {
                             const int z = pl * g.batch + tile.b;
-                            const uint32_t da = dst + pl * C::kABytes, db = dst + kLoaded * C::kABytes + pl * C::kBBytes;
+                            const uint32_t da = dst + pl * C::kABytes, db = dst + 2 * C::kABytes + pl * C::kBBytes;
 #pragma unroll
                             for (int i = 0; i < kTileM / 64; ++i) {
                                 const int r = row + 64 * i;
@@ -405,25 +393,23 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
                 g, f, [&](const Tile&) {
                     const uint32_t idesc = 1u << 4 | (uint32_t)f.a_mn << 15 | (uint32_t)f.b_mn << 16 | (uint32_t)(BN >> 3) << 17 | (uint32_t)(CTAS * kTileM >> 4) << 24;
                     const uint32_t ka = f.a_mn ? 2048 >> 4 : 32 >> 4, kb16 = f.b_mn ? 2048 >> 4 : 32 >> 4;   // 16 k further
-                    for (int kc = 0; kc < k_blocks; kc += chunk) {
+                    for (int kc = 0; kc < k_blocks; kc += kChunk) {
                         if (!(ok = mbar_wait(acc_empty(buf), acc_phase ^ 1, abort))) return false;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint32_t d = tmem + buf * BN;
-                        for (int kb = kc; kb < min(kc + chunk, k_blocks); ++kb) {
+                        for (int kb = kc; kb < min(kc + kChunk, k_blocks); ++kb) {
                             if (!(ok = mbar_wait(full(ring.stage), ring.phase, abort))) return false;
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                            const uint32_t sa = smem_addr(base) + ring.stage * kStageBytes, sb = sa + kLoaded * C::kABytes;
+                            const uint32_t sa = smem_addr(base) + ring.stage * kStageBytes, sb = sa + 2 * C::kABytes;
                             const uint64_t a_hi = operand_desc(sa, f.a_mn), b_hi = operand_desc(sb, f.b_mn);
-                            if constexpr (PROD == 3) {   // the small terms first, while the accumulator is small
-                                const uint64_t a_lo = operand_desc(sa + C::kABytes, f.a_mn), b_lo = operand_desc(sb + C::kBBytes, f.b_mn);
+                            const uint64_t a_lo = operand_desc(sa + C::kABytes, f.a_mn), b_lo = operand_desc(sb + C::kBBytes, f.b_mn);
 #pragma unroll
-                                for (int k = 0; k < kTileK / 16; ++k) {
-                                    mma_f16<CTAS>(d, a_hi + k * ka, b_lo + k * kb16, idesc, kb > kc || k > 0);
-                                    mma_f16<CTAS>(d, a_lo + k * ka, b_hi + k * kb16, idesc, true);
-                                }
+                            for (int k = 0; k < kTileK / 16; ++k) {   // the small terms first, while the accumulator is small
+                                mma_f16<CTAS>(d, a_hi + k * ka, b_lo + k * kb16, idesc, kb > kc || k > 0);
+                                mma_f16<CTAS>(d, a_lo + k * ka, b_hi + k * kb16, idesc, true);
                             }
 #pragma unroll
-                            for (int k = 0; k < kTileK / 16; ++k) mma_f16<CTAS>(d, a_hi + k * ka, b_hi + k * kb16, idesc, PROD == 3 || kb > kc || k > 0);
+                            for (int k = 0; k < kTileK / 16; ++k) mma_f16<CTAS>(d, a_hi + k * ka, b_hi + k * kb16, idesc, true);
                             mma_commit<CTAS>(empty(ring.stage));
                             if (++ring.stage == kStages) ring.stage = 0, ring.phase ^= 1;
                         }
@@ -492,7 +478,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
                         __syncwarp();
                     }
                 }
-                for (int kc = 0; kc < k_blocks; kc += chunk) {
+                for (int kc = 0; kc < k_blocks; kc += kChunk) {
                     ok &= mbar_wait(acc_full(buf), acc_phase, abort);
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     if (ok) {
@@ -1258,33 +1244,30 @@ struct Device {
     cudaStream_t stream;
 };
 
-template <int CTAS, int BN, int MODE, int PROD>
+template <int CTAS, int BN, int MODE>
 int launch_ns(const NsParams& g, int units, const Device& d) {
     using C = Config<CTAS, BN>;
     static std::atomic<uint64_t> allowed{0};
     const uint64_t bit = 1ull << (d.dev & 63);
     if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        if (cudaFuncSetAttribute(ns_kernel<CTAS, BN, MODE, PROD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem) != cudaSuccess) return HPL_ERR_CUDA;
+        if (cudaFuncSetAttribute(ns_kernel<CTAS, BN, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::kSmem) != cudaSuccess) return HPL_ERR_CUDA;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
-    return launch(ns_kernel<CTAS, BN, MODE, PROD>, dim3(CTAS * g.split * units), kGemmThreads, C::kSmem, CTAS * g.split, d.stream, g);
+    return launch(ns_kernel<CTAS, BN, MODE>, dim3(CTAS * g.split * units), kGemmThreads, C::kSmem, CTAS * g.split, d.stream, g);
 }
 template <int CTAS, int BN>
 int launch_phase(const NsParams& g, int units, const Device& d) {
     const Phase f = phase_at(g, g.phase, CTAS * kTileM, BN);
     const int mode = !f.dst ? kFinal : f.src ? kAddend : kPlanes;
-    if (f.prod == 3)
-        return mode == kPlanes ? launch_ns<CTAS, BN, kPlanes, 3>(g, units, d) : mode == kAddend ? launch_ns<CTAS, BN, kAddend, 3>(g, units, d) : launch_ns<CTAS, BN, kFinal, 3>(g, units, d);
-    return mode == kPlanes ? launch_ns<CTAS, BN, kPlanes, 1>(g, units, d) : mode == kAddend ? launch_ns<CTAS, BN, kAddend, 1>(g, units, d) : launch_ns<CTAS, BN, kFinal, 1>(g, units, d);
+    return mode == kPlanes ? launch_ns<CTAS, BN, kPlanes>(g, units, d) : mode == kAddend ? launch_ns<CTAS, BN, kAddend>(g, units, d) : launch_ns<CTAS, BN, kFinal>(g, units, d);
 }
 // Tiles of 256 x 256 on pairs of CTAs keep the tensor cores busiest (operands from L2 once per 256 rows and columns); 128 x 128
 // and 128 x 64 give more SMs work where the matrix is small.
 struct Kind {
     int ctas, bn;
-    int block[2], tile[2], once[2];     // measured clocks of single and triple products: 64 k; a tile beside its products; a launch's end
+    int block, tile, once;     // measured clocks: 64 k; a tile beside its products; a launch's end
 };
-constexpr Kind kKinds[3] = {{2, 256, {740, 1750}, {2000, 20000}, {18000, 4000}}, {1, 128, {600, 1250}, {3000, 9000}, {9000, 4000}},
-                            {1, 64, {560, 1200}, {2500, 6000}, {7500, 4000}}};
+constexpr Kind kKinds[3] = {{2, 256, 1750, 20000, 4000}, {1, 128, 1250, 9000, 4000}, {1, 64, 1200, 6000, 4000}};
 constexpr int kMeet = 9000, kMaxSplit = 8;       // what it takes to bring parts of a sum together; parts at most
 
 int64_t rounds(int64_t work, int64_t by) { return (work + by - 1) / by; }
@@ -1302,8 +1285,7 @@ Plan plan_phase(const NsParams& g, int sms) {
         const int64_t tiles = (int64_t)f.tiles * g.batch, blocks = (f.K + kTileK - 1) / kTileK;
         for (int split = 1; split <= (k.ctas == 1 ? kMaxSplit : 1) && split <= blocks && (split == 1 || tiles * split <= (split == 2 ? sms : sms * 7 / 8)); ++split) {
             if (rounds(blocks, rounds(blocks, split)) != split) continue;       // the last part would be empty
-            const int w = f.prod == 3;
-            const int64_t t = rounds(tiles, sms / k.ctas) * (rounds(blocks, split) * k.block[w] + k.tile[w]) + k.once[w] + (split > 1 ? kMeet : 0);
+            const int64_t t = rounds(tiles, sms / k.ctas) * (rounds(blocks, split) * k.block + k.tile) + k.once + (split > 1 ? kMeet : 0);
             if (t < best.time) best = {i, split, tiles, t};
         }
     }
@@ -1423,7 +1405,6 @@ int orthogonalize(const Problem& q, UpdateParams u, Output out, cudaStream_t str
     g.side = (int32_t)lay.side;
     g.batch = (int32_t)q.batch;
     g.steps = q.steps;
-    g.single = out.bf16 && lay.side > kSingleSide;
     return run_steps(g, d);
 }
 
