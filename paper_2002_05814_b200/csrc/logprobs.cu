@@ -607,7 +607,7 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const LogprobsParams p) {
     Running run;
     bool ok = true;
     for (int i = 0, v = tid; v < nv; ++i, v += kChunkVecs) {
-        if (!(ok = mbar_wait(bar0 + 8 * i, 0, &abort_flag))) break;
+        if (!(ok = mbar_wait(bar0 + 8 * i, 0, &abort_flag, kResults))) break;
         if (v + (kBatch - 1) * kThreads < nv) {
             uint4 w[kBatch];
 #pragma unroll
@@ -727,7 +727,7 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
             const RowShape shape = row_shape<BF16>(x_row, p.vocab);
             const char* src = x_row + shape.head * E::kBytes;
             for (int v = 0; v < shape.vecs; v += kChunkVecs) {
-                if (!mbar_wait(empty0 + 8 * slot, phase ^ 1, &sh.abort_flag)) {
+                if (!mbar_wait(empty0 + 8 * slot, phase ^ 1, &sh.abort_flag, kLoads)) {
                     let_copies_land();
                     return;
                 }
@@ -758,7 +758,7 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
         Running run;
         bool ok = true;
         for (int v = 0, n = 0; v < shape.vecs; v += kChunkVecs, ++n) {
-            ok &= mbar_wait(full0 + 8 * slot, phase, &sh.abort_flag);
+            ok &= mbar_wait(full0 + 8 * slot, phase, &sh.abort_flag, kResults);
             const uint4* in = slots + slot * kChunkVecs;
             const int left = shape.vecs - v - tid;       // this thread's vectors: those of 0, 256, 512, 768 below it
             float most[kBatch];
@@ -1070,6 +1070,7 @@ int run_pass(const hpl_logprobs_args* a, Pass pass, cudaStream_t stream) {
         p.d_logits = a->d_logits;
         p.d_row_stride = d_stride;
     }
+    if (!arm_expiry(stream)) return HPL_ERR_CUDA;
     const bool bf16 = a->dtype == HPL_BF16;
     if (a->vocab <= kSmallVocab) return bf16 ? launch_small_any<true>(p, pass == kBackward, stream) : launch_small_any<false>(p, pass == kBackward, stream);
     if (pass == kBackward) return bf16 ? launch_grad<true>(p, stream) : launch_grad<false>(p, stream);

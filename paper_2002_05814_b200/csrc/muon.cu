@@ -356,13 +356,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
     if (warp >= kEpiWarps) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");      // 128 * 88 + 256 * 208 = 384 * 168
         if (warp == 8 && lane == 0) {
-            bool ok = true;
             walk<CTAS, BN>(
                 g, f, [&](const Tile& tile) {
                     const int row = tile.row + (int)cta * kTileM, col = tile.col + (int)cta * C::kBRows;
                     for (int kb = 0; kb < k_blocks; ++kb) {
                         const int k0 = (first_block + kb) * kTileK;
-                        if (!(ok = mbar_wait(empty(ring.stage), ring.phase ^ 1, abort))) return false;
+                        if (!mbar_wait(empty(ring.stage), ring.phase ^ 1, abort, kLoads)) return false;
                         const uint32_t dst = smem_addr(base) + ring.stage * kStageBytes;
                         const uint32_t bar = CTAS == 2 ? leader_addr(full(ring.stage)) : full(ring.stage);
                         if (cta == 0) mbar_expect(full(ring.stage), CTAS * kStageBytes);
@@ -384,21 +383,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
                     }
                     return true;
                 });
-            if (!ok) let_copies_land();
         } else if (warp == 9 && lane == 0 && cta == 0) {
             int buf = 0;
             uint32_t acc_phase = 0;
-            bool ok = true;
             walk<CTAS, BN>(
                 g, f, [&](const Tile&) {
                     const uint32_t idesc = 1u << 4 | (uint32_t)f.a_mn << 15 | (uint32_t)f.b_mn << 16 | (uint32_t)(BN >> 3) << 17 | (uint32_t)(CTAS * kTileM >> 4) << 24;
                     const uint32_t ka = f.a_mn ? 2048 >> 4 : 32 >> 4, kb16 = f.b_mn ? 2048 >> 4 : 32 >> 4;   // 16 k further
                     for (int kc = 0; kc < k_blocks; kc += kChunk) {
-                        if (!(ok = mbar_wait(acc_empty(buf), acc_phase ^ 1, abort))) return false;
+                        if (!mbar_wait(acc_empty(buf), acc_phase ^ 1, abort, kProducts)) return false;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint32_t d = tmem + buf * BN;
                         for (int kb = kc; kb < min(kc + kChunk, k_blocks); ++kb) {
-                            if (!(ok = mbar_wait(full(ring.stage), ring.phase, abort))) return false;
+                            if (!mbar_wait(full(ring.stage), ring.phase, abort, kProducts)) return false;
                             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                             const uint32_t sa = smem_addr(base) + ring.stage * kStageBytes, sb = sa + 2 * C::kABytes;
                             const uint64_t a_hi = operand_desc(sa, f.a_mn), b_hi = operand_desc(sb, f.b_mn);
@@ -479,9 +476,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
                     }
                 }
                 for (int kc = 0; kc < k_blocks; kc += kChunk) {
-                    ok &= mbar_wait(acc_full(buf), acc_phase, abort);
-                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    // A warp that has given up reads no more and frees no accumulator: what it has not read may not be overwritten, for
+                    // the other CTA of a pair may still be right.  The warp as a whole: its loads are aligned ones.
+                    if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(acc_full(buf), acc_phase, abort, kResults));
                     if (ok) {
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
                         for (int q = 0; q < kCols; q += 32) {
                             uint32_t v[32];
@@ -489,12 +488,12 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
 #pragma unroll
                             for (int i = 0; i < 16; ++i) add_pair(acc[q / 2 + i], v[2 * i], v[2 * i + 1]);
                         }
-                    }
-                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (CTAS == 2) mbar_arrive_remote(leader_addr(acc_empty(buf)));
-                        else mbar_arrive(acc_empty(buf));
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (CTAS == 2) mbar_arrive_remote(leader_addr(acc_empty(buf)));
+                            else mbar_arrive(acc_empty(buf));
+                        }
                     }
                     buf ^= 1;
                     if (buf == 0) acc_phase ^= 1;
@@ -610,6 +609,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
         meet<2>();
     }
     __syncthreads();
+    if (*abort) let_copies_land();          // loads into the ring and products that nobody waited for
     if constexpr (CTAS == 2) meet<2>();     // neither leaves while the other may still signal it
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     if (warp == 9) {
@@ -945,7 +945,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const SmallPara
             issue();
             mma_commit<1>(done);
         }
-        ok &= mbar_wait(done, phase, &abort_flag);
+        ok &= mbar_wait(done, phase, &abort_flag, kResults);
         phase ^= 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     };
@@ -1362,7 +1362,7 @@ int orthogonalize(const Problem& q, UpdateParams u, Output out, cudaStream_t str
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return HPL_ERR_CUDA;
     EncodeFn f = encode_fn();
-    if (!f) return HPL_ERR_CUDA;
+    if (!f || !arm_expiry(stream)) return HPL_ERR_CUDA;
     uint8_t* ws = (uint8_t*)up((int64_t)(uintptr_t)q.workspace, 256);
     Planes x[2], a, p;
     for (int i = 0; i < 2; ++i) x[i] = {(__half*)(ws + lay.off_x[i]), lay.x_plane, q.rows * lay.ldx, (int32_t)lay.ldx};

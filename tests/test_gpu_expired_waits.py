@@ -1,0 +1,79 @@
+"""Device waits of the learner operators that run out: the kernels end, what depended on the wait is NaN and nothing is finite and
+wrong, and the next call is right.
+
+The bounds-checking build lets the waits of one kind in one block run out (HPL_DEBUG_EXPIRE=<waiter>,<block>,<n>: all but the first n
+of the call's), whatever they wait for; the block's other waits, and those of other blocks on it, then reach their own limit.  Each group
+runs in a process of its own, with that build.
+"""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+LOADS, PRODUCTS, RESULTS = 1, 2, 3
+
+
+def _expire(waiter=0, block=0, after=0):
+    os.environ["HPL_DEBUG_EXPIRE"] = f"{waiter},{block},{after}"
+
+
+def _ortho(hpl, torch, u, dtype, steps):
+    batch, rows, cols = u.shape
+    ws = torch.empty(hpl.orthogonalize_workspace(batch, rows, cols), dtype=torch.uint8, device="cuda")
+    out = torch.full((batch, rows, cols), 777.0, dtype=dtype, device="cuda")
+    hpl.orthogonalize(hpl.OrthoArgs(src=u.data_ptr(), dst=out.data_ptr(), dst_dtype=hpl.HPL_BF16 if dtype == torch.bfloat16 else hpl.HPL_F32,
+                                    batch=batch, rows=rows, cols=cols, steps=steps, workspace=ws.data_ptr(), workspace_bytes=ws.numel()),
+                      torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+    return out
+
+
+def _check_products(batch, rows, cols, blocks, waiters, counts):
+    """An element is NaN or the one of an undisturbed call, bit for bit; from the first wait on, some are NaN."""
+    import torch
+
+    import paper_2002_05814_b200 as hpl
+    u = torch.randn(batch, rows, cols, device="cuda", generator=torch.Generator(device="cuda").manual_seed(rows))
+    for dtype, steps in ((torch.float32, 1), (torch.bfloat16, 2)):
+        _expire()
+        right = _ortho(hpl, torch, u, dtype, steps)
+        assert torch.isfinite(right).all()
+        for waiter in waiters:
+            for block in blocks:
+                for after in counts:
+                    _expire(waiter, block, after)
+                    got = _ortho(hpl, torch, u, dtype, steps)
+                    nan = torch.isnan(got)
+                    what = f"{batch} x {rows} x {cols}, {dtype}, waiter {waiter} of block {block} after {after}"
+                    assert (nan | (got == right)).all(), f"{what}: {(~nan & (got != right)).sum().item()} elements finite and wrong"
+                    assert after or nan.any(), what
+                    _expire()
+                    assert torch.equal(_ortho(hpl, torch, u, dtype, steps), right), f"the call after {what}"
+
+
+def products():
+    """Tiles on a CTA and on a pair, by themselves (a pair's second CTA starts no products)."""
+    _check_products(1, 300, 500, (0, 7), (LOADS, PRODUCTS, RESULTS), (0, 9, 40, 1500))
+    _check_products(2, 2048, 2048, (0,), (LOADS, PRODUCTS, RESULTS), (0, 40, 9000))
+    _check_products(2, 2048, 2048, (1,), (LOADS, RESULTS), (0, 40, 9000))
+
+
+GROUPS = {f.__name__: f for f in (products,)}
+
+
+@pytest.mark.parametrize("group", sorted(GROUPS))
+def test_expired_waits(group):
+    env = dict(os.environ, HPL_DEBUG_BOUNDS="1")
+    build = subprocess.run([sys.executable, "-m", "paper_2002_05814_b200.build"], cwd=ROOT, env=env, capture_output=True, text=True)
+    assert build.returncode == 0, build.stderr[-2000:]
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), group], cwd=ROOT, env=env, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+if __name__ == "__main__":
+    sys.path.insert(0, ROOT)
+    GROUPS[sys.argv[1]]()
