@@ -500,6 +500,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) ns_kernel(const __grid_consta
                 }
                 if (CTAS == 1 && g.split > 1) {
                     // the parts come together in the first CTA, in order; the ring has been read to its end and holds them meanwhile
+                    if (!ok) {                         // ... or loads may be on their way to it
+                        let_copies_land();
+#pragma unroll
+                        for (int i = 0; i < kCols / 2; ++i) acc[i] = 0x7FC000007FC00000ull;     // the sum is to be NaN
+                    }
                     ulonglong2* mine = (ulonglong2*)base + threadIdx.x;
                     if (part)
 #pragma unroll

@@ -62,7 +62,13 @@ def products():
     _check_products(2, 2048, 2048, (1,), (LOADS, RESULTS), (0, 40, 9000))
 
 
-GROUPS = {f.__name__: f for f in (products,)}
+def shared_sums():
+    """Sums over k that the CTAs of a cluster share: a part that gives up, whichever it is, makes the sum NaN."""
+    _check_products(1, 333, 1000, (0, 1, 7, 30), (LOADS, PRODUCTS, RESULTS), (0, 1, 3, 300))
+    _check_products(1, 1024, 4096, (0, 1, 2, 106), (LOADS, PRODUCTS, RESULTS), (0, 5, 700))
+
+
+GROUPS = {f.__name__: f for f in (products, shared_sums)}
 
 
 @pytest.mark.parametrize("group", sorted(GROUPS))
