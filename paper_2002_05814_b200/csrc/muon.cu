@@ -950,7 +950,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) small_kernel(const SmallPara
             issue();
             mma_commit<1>(done);
         }
-        ok &= mbar_wait(done, phase, &abort_flag, kResults);
+        if (!mbar_wait(done, phase, &abort_flag, kResults)) {
+            ok = false;
+            let_copies_land();                                      // its operands and its accumulators are used again
+        }
+        __syncwarp();                                               // the loads of accumulators are aligned ones
         phase ^= 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     };

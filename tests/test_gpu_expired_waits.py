@@ -68,7 +68,14 @@ def shared_sums():
     _check_products(1, 1024, 4096, (0, 1, 2, 106), (LOADS, PRODUCTS, RESULTS), (0, 5, 700))
 
 
-GROUPS = {f.__name__: f for f in (products, shared_sums)}
+def small_matrices():
+    """Everything in one launch, on a CTA and on a cluster."""
+    _check_products(3, 64, 128, (0, 2), (RESULTS,), (0, 100, 256, 700, 1000))
+    _check_products(1, 128, 2048, (0, 5), (RESULTS,), (0, 100, 256, 700, 1000))
+    _check_products(2, 600, 50, (0, 2), (RESULTS,), (0, 100, 256, 700, 1000))
+
+
+GROUPS = {f.__name__: f for f in (products, shared_sums, small_matrices)}
 
 
 @pytest.mark.parametrize("group", sorted(GROUPS))
