@@ -737,10 +737,12 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
                 advance();
             }
         }
+        if (*(volatile int*)&sh.abort_flag) let_copies_land();     // nobody may be waiting for them
         return;
     }
     const float c = p.scale_log2e;
     int parity = 0;
+    bool ok = true;        // for good: once a wait has run out, this thread no longer knows which pass of the ring a slot holds
     for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x, parity ^= 1) {
         const char* x_row = (const char*)p.logits + row * p.row_stride * E::kBytes;
         const RowShape shape = row_shape<BF16>(x_row, p.vocab);
@@ -756,9 +758,8 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
             if (has_token) token_x = E::load(x_row, t);
         }
         Running run;
-        bool ok = true;
         for (int v = 0, n = 0; v < shape.vecs; v += kChunkVecs, ++n) {
-            ok &= mbar_wait(full0 + 8 * slot, phase, &sh.abort_flag, kResults);
+            if (ok) ok = mbar_wait(full0 + 8 * slot, phase, &sh.abort_flag, kResults);
             const uint4* in = slots + slot * kChunkVecs;
             const int left = shape.vecs - v - tid;       // this thread's vectors: those of 0, 256, 512, 768 below it
             float most[kBatch];
@@ -767,7 +768,7 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
 #pragma unroll
                 for (int i = 0; i < kBatch; ++i) w[i] = in[tid + i * kThreads];
                 __syncwarp();
-                if (lane == 0) mbar_arrive(empty0 + 8 * slot);
+                if (lane == 0 && ok) mbar_arrive(empty0 + 8 * slot);
                 if (runs == 1) {
                     most[0] = run.add<BF16, kBatch>(w, c);
                 } else {
@@ -781,7 +782,7 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
                     if (i * kThreads < left) most[i] = run.add<BF16, 1>({in[tid + i * kThreads]}, c);
                 }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(empty0 + 8 * slot);
+                if (lane == 0 && ok) mbar_arrive(empty0 + 8 * slot);
                 if (runs == 1) most[0] = max_nan(max_nan(most[0], most[1]), max_nan(most[2], most[3]));
             }
             if (p.top_k) {
@@ -827,7 +828,8 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
             if (lane == 0) atomicMin(&sh.bound_value, least);
             consumers_sync();
         }
-        uint64_t bound = entries >= p.top_k ? (uint64_t)sh.bound_value << 32 : 0;
+        // (after a wait that ran out the entries say nothing: all of the row is looked through)
+        uint64_t bound = entries >= p.top_k && !*(volatile int*)&sh.abort_flag ? (uint64_t)sh.bound_value << 32 : 0;
         for (int e = tid; e < entries; e += kThreads)
             if (sh.entry[e] >= (uint32_t)(bound >> 32)) sh.winners[atomicAdd(&sh.n_winners, 1u)] = (uint16_t)e;
         consumers_sync();
@@ -892,6 +894,7 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
             }
         } while (over);
     }
+    if (!ok) let_copies_land();
 }
 
 // ------------------------------------------------------------------ gradient from saved statistics

@@ -75,7 +75,61 @@ def small_matrices():
     _check_products(2, 600, 50, (0, 2), (RESULTS,), (0, 100, 256, 700, 1000))
 
 
-GROUPS = {f.__name__: f for f in (products, shared_sums, small_matrices)}
+def _check_rows(rows, vocab, dtype, k, gradient, blocks, waiters, counts):
+    """A row is right, or NaN as a whole; its alternatives are found either way.  From the first wait on, some are NaN."""
+    import torch
+
+    import paper_2002_05814_b200 as hpl
+    gen = torch.Generator(device="cuda").manual_seed(vocab)
+    x = torch.randn(rows, vocab, device="cuda", generator=gen).to(dtype)
+    t = torch.randint(0, vocab, (rows,), device="cuda", generator=gen)
+    g, h = torch.randn(rows, device="cuda", generator=gen), torch.randn(rows, device="cuda", generator=gen)
+
+    def call():
+        out = {n: torch.full((rows, w), 777.0, device="cuda") for n, w in (("logprob", 1), ("entropy", 1), ("row_stats", 4), ("top_logprob", k))}
+        index = torch.full((rows, k), 777, dtype=torch.int64, device="cuda")
+        a = hpl.LogprobsArgs(logits=x.data_ptr(), dtype=hpl.HPL_BF16 if dtype == torch.bfloat16 else hpl.HPL_F32, rows=rows, vocab=vocab,
+                             targets=t.data_ptr(), top_k=k, top_index=index.data_ptr() if k else 0)
+        for name, v in out.items():
+            if v.numel():
+                setattr(a, name, v.data_ptr())
+        if gradient:
+            out["d_logits"] = torch.full((rows, vocab), 777.0, dtype=dtype, device="cuda")
+            a.d_logprob, a.d_entropy, a.d_logits = g.data_ptr(), h.data_ptr(), out["d_logits"].data_ptr()
+        (hpl.token_logprobs_with_grad if gradient else hpl.token_logprobs)(a, torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+        out["row_stats"] = out["row_stats"][:, 1:]               # the maximum may be of a part
+        return out, index
+
+    _expire()
+    right, order = call()
+    assert all(torch.isfinite(v).all() for v in right.values())
+    for waiter in waiters:
+        for block in blocks:
+            for after in counts:
+                _expire(waiter, block, after)
+                got, index = call()
+                what = f"{rows} x {vocab}, {dtype}, waiter {waiter} of block {block} after {after}"
+                given_up = torch.isnan(got["logprob"][:, 0])
+                for name, v in got.items():
+                    assert torch.isnan(v[given_up]).all(), f"{what}: {name} of a row given up"
+                    assert torch.equal(v[~given_up], right[name][~given_up]), f"{what}: {name}, finite and wrong"
+                assert torch.equal(index, order), what
+                assert after or given_up.any(), what
+                _expire()
+                again, index = call()
+                assert all(torch.equal(v, right[name]) for name, v in again.items()) and torch.equal(index, order), f"the call after {what}"
+
+
+def streamed_rows():
+    """Many rows through a ring: those after one that was given up hold nothing of an earlier pass of the ring."""
+    import torch
+    for k in (0, 8):
+        _check_rows(1500, 70_003, torch.bfloat16, k, False, (0, 300), (LOADS, RESULTS), (0, 5, 1000, 9000))
+    _check_rows(1500, 33_001, torch.float32, 3, False, (5,), (LOADS, RESULTS), (0, 7, 2500))
+
+
+GROUPS = {f.__name__: f for f in (products, shared_sums, small_matrices, streamed_rows)}
 
 
 @pytest.mark.parametrize("group", sorted(GROUPS))
