@@ -607,7 +607,10 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const LogprobsParams p) {
     Running run;
     bool ok = true;
     for (int i = 0, v = tid; v < nv; ++i, v += kChunkVecs) {
-        if (!(ok = mbar_wait(bar0 + 8 * i, 0, &abort_flag, kResults))) break;
+        if (!(ok = mbar_wait(bar0 + 8 * i, 0, &abort_flag, kResults))) {
+            let_copies_land();       // what follows reads all of them: the alternatives' bound, the search, the gradient
+            break;
+        }
         if (v + (kBatch - 1) * kThreads < nv) {
             uint4 w[kBatch];
 #pragma unroll
@@ -676,7 +679,6 @@ __global__ void __launch_bounds__(kThreads) row_kernel(const LogprobsParams p) {
         }
         if (single >= 0) E::store(d_row, single, grad_of(single_x, c, g) + (single == g.t ? g.token : 0.f));
     }
-    if (!ok) let_copies_land();
     if (n_ranks > 1) asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
 }
 

@@ -129,7 +129,15 @@ def streamed_rows():
     _check_rows(1500, 33_001, torch.float32, 3, False, (5,), (LOADS, RESULTS), (0, 7, 2500))
 
 
-GROUPS = {f.__name__: f for f in (products, shared_sums, small_matrices, streamed_rows)}
+def rows_on_chip():
+    """A row in the shared memory of a CTA or a cluster, with and without its gradient."""
+    import torch
+    _check_rows(5, 3000, torch.float32, 7, True, (0, 5), (RESULTS,), (0, 100, 2000))
+    _check_rows(2, 131_072, torch.bfloat16, 32, False, (0, 3, 15), (RESULTS,), (0, 200, 600))
+    _check_rows(257, 50_021, torch.bfloat16, 4, True, (0, 101), (RESULTS,), (0, 300, 1000))
+
+
+GROUPS = {f.__name__: f for f in (products, shared_sums, small_matrices, streamed_rows, rows_on_chip)}
 
 
 @pytest.mark.parametrize("group", sorted(GROUPS))
