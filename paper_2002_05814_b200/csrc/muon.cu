@@ -40,6 +40,10 @@ constexpr int kBoxBytes = 64 * 128;          // a TMA box: 64 rows of 64 fp16, 1
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = (kEpiWarps + 4) * 32;   // whole warpgroups: loads and products have one of their own
 constexpr int kBlockWords = 32 * 32;         // an epilogue warp's transposition block
+// Shared memory of an SM, and what each block takes beside its own.  A block that holds tensor memory while it waits for the others of its
+// cluster takes so much that no further block fits on its SM: two clusters could else each hold the tensor memory that a block of the other
+// waits for.  A block without a cluster waits for nothing that holds any: it may share its SM.
+constexpr size_t kSmSmem = 228 << 10, kBlockReserve = 1024;
 constexpr int kPartials = 1024;               // at most so many partial sums of squares per matrix
 
 // The three products of a step; the last one of the last step makes the result.
@@ -239,6 +243,7 @@ struct Config {
     static constexpr int kScratch = kEpiWarps * kBlockWords * 4;
     static constexpr int kRing = (227 << 10) - 1024 - 512 - kScratch;
     static constexpr size_t kSmem = 1024 + (size_t)kRing + kScratch + 512;
+    static_assert(kSmem + kBlockReserve <= kSmSmem && kSmem + 2 * kBlockReserve > kSmSmem, "a block of a cluster that takes tensor memory has the SM to itself");
     static constexpr int kStageBytes = (kABytes + kBBytes) * 2, kStages = kRing / kStageBytes;   // as many as fit: 3 or 4
 };
 
@@ -1350,12 +1355,13 @@ int launch_small(const UpdateParams& u, const Output& out, int side, int length,
     p.tall = q.rows > q.cols;
     p.steps = q.steps;
     p.cols = (int32_t)up((length + ranks - 1) / ranks, 64);
-    const size_t smem = 1024 + 2 * kBlockBytes * (size_t)(p.cols / 64 + (side + 63) / 64);
+    constexpr size_t whole = kSmSmem - 2 * kBlockReserve;              // the static part is below kBlockReserve
+    static_assert(1024 + 2 * kBlockBytes * (kSmallCols / 64 + kSmallSide / 64) <= whole, "the largest case fits");
+    const size_t smem = ranks > 1 ? whole : 1024 + 2 * kBlockBytes * (size_t)(p.cols / 64 + (side + 63) / 64);
     static std::atomic<uint64_t> allowed{0};
     const uint64_t bit = 1ull << (d.dev & 63);
     if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        constexpr size_t most = 1024 + 2 * kBlockBytes * (kSmallCols / 64 + kSmallSide / 64);
-        if (cudaFuncSetAttribute(small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most) != cudaSuccess) return HPL_ERR_CUDA;
+        if (cudaFuncSetAttribute(small_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)whole) != cudaSuccess) return HPL_ERR_CUDA;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
     return launch(small_kernel, dim3((unsigned)(q.batch * ranks)), kSmallThreads, smem, ranks, d.stream, p);
