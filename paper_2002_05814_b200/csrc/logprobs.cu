@@ -481,7 +481,7 @@ __device__ void top_of_segment(TopScratch& t, const uint4* seg, int nv, uint32_t
     for (int o = 1; o < kPer; o <<= 1) gm = max(gm, __shfl_xor_sync(0xFFFFFFFFu, gm, o));
     if (tid % kPer == 0) t.group_max[tid / kPer] = gm;
     if (tid < HPL_TOP_MAX) t.list[tid] = 0;
-    if (tid == 0) t.n = t.n_winners = 0, t.bound_value = 0xFFFFFFFFu;
+    if (tid == 0) t.n = 0, t.bound_value = 0xFFFFFFFFu;
     __syncthreads();
     if (tid < kGroups) {        // the k-th largest is the least that fewer than k exceed
         const uint32_t mine = t.group_max[tid];
@@ -496,7 +496,13 @@ __device__ void top_of_segment(TopScratch& t, const uint4* seg, int nv, uint32_t
     }
     __syncthreads();
     uint64_t bound = (uint64_t)t.bound_value << 32;
-    if (tid < kGroups && t.group_max[tid] >= (uint32_t)(bound >> 32)) t.winners[atomicAdd(&t.n_winners, 1u)] = tid;
+    if (tid < kGroups) {        // in order: among ties the first gathered are then low indices, which makes for a good next bound
+        const uint32_t least = (uint32_t)(bound >> 32);
+        const uint32_t first = __ballot_sync(0xFFFFFFFFu, t.group_max[tid % 32] >= least), second = __ballot_sync(0xFFFFFFFFu, t.group_max[32 + tid % 32] >= least);
+        const uint32_t mine = tid < 32 ? first : second, bit = 1u << tid % 32;
+        if (mine & bit) t.winners[__popc(mine & (bit - 1)) + (tid < 32 ? 0 : __popc(first))] = tid;
+        if (tid == 0) t.n_winners = __popc(first) + __popc(second);
+    }
     __syncthreads();
     const int per_group = kPer * ((nv + kThreads - 1) / kThreads), work = (int)t.n_winners * per_group;
     for (;;) {
