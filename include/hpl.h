@@ -384,7 +384,8 @@ int hpl_reduce_noalloc(const void* const* src_bufs, int32_t n, int32_t degree, i
  * and, for upstream gradients g = d_logprob, h = d_entropy,
  *     d_logits_j = scale * ( g (delta_jt - p_j) - h p_j (log p_j + entropy) ).
  * A token that is not in [0, vocab) is no token: its logprob is 0 and it has no gradient.  Logits of -inf are masked:
- * probability 0, gradient 0.  A row with nothing but -inf has logprob and top_logprob -inf, entropy 0, gradient 0.
+ * probability 0, gradient 0 -- but for the row's own token: one whose logit is -inf (logprob -inf) still has the term scale * g at its
+ * place, as the formula says, so a caller who does not want it passes g = 0 or no token.  A row with nothing but -inf has logprob and top_logprob -inf, entropy 0, gradient 0.
  * NaN or +inf in a row makes the row's results NaN (of the alternatives' order, NaN ranks above +inf).  Arithmetic and statistics are fp32 for either type of logits. */
 #define HPL_TOP_MAX                32
 #define HPL_LOGPROBS_MAX_ROWS      (1ll << 25)
