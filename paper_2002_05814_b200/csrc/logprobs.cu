@@ -906,7 +906,7 @@ __global__ void __launch_bounds__(kStreamThreads) stream_kernel(const LogprobsPa
 }
 
 // ------------------------------------------------------------------ gradient from saved statistics
-// CTA (x, y): segment x of row y (rows beyond 65535 in strides).  Eight vectors per thread, four loads in flight at a time.
+// Block i: part i % segs of row i / segs.  Eight vectors per thread, four loads in flight at a time.
 constexpr int kGradVecs = 8;
 template <bool BF16>
 __global__ void __launch_bounds__(kThreads) grad_kernel(const LogprobsParams p, const uint32_t segs) {

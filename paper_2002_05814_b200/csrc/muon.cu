@@ -679,7 +679,7 @@ __device__ __forceinline__ float4 grad4(const UpdateParams& u, int64_t at, int n
 __device__ __forceinline__ float4 fma4(float a, float4 x, float4 y) { return make_float4(fmaf(a, x.x, y.x), fmaf(a, x.y, y.y), fmaf(a, x.z, y.z), fmaf(a, x.w, y.w)); }
 __device__ __forceinline__ float4 scale4(float a, float4 x) { return make_float4(a * x.x, a * x.y, a * x.z, a * x.w); }
 
-// Both kernels go over a matrix in groups of four columns; a thread has kGroups of them in flight.
+// Both kernels go over a matrix in groups of four columns; a thread has kInFlight of them in flight.
 constexpr int kInFlight = 4;
 
 // New momentum, and partial sums of the squares of U.  They are fp64: neither the squares of large nor of small updates leave
